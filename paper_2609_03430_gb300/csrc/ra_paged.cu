@@ -136,7 +136,9 @@ __device__ __forceinline__ uint32_t from_codes(uint32_t two, float scale)
 // What a CTA's first steps read: the tables, and of one-row calls the rows.
 __device__ __forceinline__ void prefetch_start(const PagedRowsParams& p, int D)
 {
-    const int i = (blockIdx.y * gridDim.x + blockIdx.x) * blockDim.x + threadIdx.x, n = gridDim.x * gridDim.y * blockDim.x;
+    const PrefetchShare mine = prefetch_share(gridDim.x, gridDim.y, blockIdx.x, blockIdx.y, blockDim.x, threadIdx.x);
+    const int i = mine.i, n = mine.n;
+    if (i < 0) return;
     prefetch_sequences(p.c, i, n);
     if (p.rows) {
         prefetch_lines(p.rows, 4ll * (p.c.batch + 1), i, n);

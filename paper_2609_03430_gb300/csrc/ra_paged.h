@@ -11,6 +11,7 @@ namespace ra {
 
 constexpr int kPagedErrInput = 4;  // value of the device error word: a length, row count or page outside its range
 constexpr int kPagedPrefetchTable = 128 << 10;  // bytes of tables that are brought into L2 ahead of their use
+constexpr int kPagedPrefetchCtas = 512;         // CTAs of a launch that bring them (a CTA per row of the largest batch)
 constexpr int kPagedMaxG = 16;     // query heads per KV head (the rows of one mma.sync operand)
 
 // Exponents of the power-of-two scales, stored as e + 127.  8-bit rows: the smallest 2^e with max |x| <= 448 * 2^e;
@@ -101,6 +102,19 @@ cudaError_t paged_attn_prepare_fp8(int D, int page, int G);
 size_t paged_partial_bytes_bf16(int G, int D, int sms);
 size_t paged_partial_bytes_fp8(int G, int D, int sms);
 cudaError_t launch_paged_attn_fp8(int D, const PagedAttnParams& p, int sms, cudaStream_t s);
+
+// Which lines thread `thread` of CTA (x, y) brings into L2 ahead: those of thread i of n, none where i < 0.  Only a launch's
+// first CTAs take part: a grid sized by a caller's upper bound on rows may hold more threads than 32 bits count, and
+// the CTAs behind the first find the lines in L2 anyway.
+struct PrefetchShare {
+    int i, n;
+};
+__host__ __device__ inline PrefetchShare prefetch_share(unsigned grid_x, unsigned grid_y, unsigned x, unsigned y, int threads, int thread)
+{
+    const unsigned long long ctas = (unsigned long long)grid_x * grid_y, cta = (unsigned long long)y * grid_x + x;
+    const int most = ctas < (unsigned long long)kPagedPrefetchCtas ? (int)ctas : kPagedPrefetchCtas;
+    return PrefetchShare{cta < (unsigned long long)most ? (int)cta * threads + thread : -1, most * threads};
+}
 
 #ifdef __CUDACC__
 // Brings lines into L2 ahead of their first use (thread i of n, before the kernel waits for its predecessor: L2 is
