@@ -116,8 +116,9 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x)
 }
 
 // The reference of a head's weights is set kBelow under the largest so far (log2 units) and moves (what is summed
-// being rescaled) only when one could pass it by kHigh.  8 bits: weights fill f16's range.
-constexpr float kHigh = RA_PAGED_FMT == 1 ? 14.f : 8.f, kBelow = RA_PAGED_FMT == 1 ? 6.f : 0.f;
+// being rescaled) only when one could pass it by kHigh.  8 bits: weights fill f16's range.  bf16: they stay in (2^-8, 1] at
+// the largest, as V rows of up to 2^128 times more than 1 would leave 32 bits.
+constexpr float kHigh = RA_PAGED_FMT == 1 ? 14.f : 0.f, kBelow = RA_PAGED_FMT == 1 ? 6.f : -8.f;
 
 // A record: o [G][D] (not divided), m [G], l [G], whether any row counted; floats, a multiple of 4.
 __host__ __device__ constexpr int record_floats(int G, int D) { return G * D + (2 * G + 1 + 3) / 4 * 4; }
