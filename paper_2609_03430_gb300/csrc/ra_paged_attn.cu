@@ -10,7 +10,7 @@
 //   bf16:  weights in two bf16 parts (nearest, and what that left out), in products of their own.
 //   8 bits: codes become f16 (exactly) in registers, queries f16 at a power of two of their row (exactly, but for
 //          channels below 2^-38 of the largest), weights f16.  A row's power-of-two scales go to its logit (K) and its
-//          weight (V); the reference of the weights follows logit + log2 of the V scale, so that a weight fits f16
+//          weight (V); the unit of the sums of values follows logit + log2 of the V scale, so that a weight fits f16
 //          whatever the scale.  (8-bit operands, queries in three parts, took more instructions than the kernel then
 //          had, 808 per tile of 32 rows against 603; it has 443 now.)
 // A head that lies in one share is written by its warp; the parts of the others go to records that a second kernel
@@ -115,13 +115,18 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x)
     return y;
 }
 
-// The reference of a head's weights is set kBelow under the largest so far (log2 units) and moves (what is summed
-// being rescaled) only when one could pass it by kHigh.  8 bits: weights fill f16's range.  bf16: they stay in (2^-8, 1] at
-// the largest, as V rows of up to 2^128 times more than 1 would leave 32 bits.
-constexpr float kHigh = RA_PAGED_FMT == 1 ? 14.f : 0.f, kBelow = RA_PAGED_FMT == 1 ? 6.f : -8.f;
+// The reference m of a head's weights is set kAbove over the largest logit so far (log2 units) and moves (what is summed
+// being rescaled) only when one passes it: weights stay at or below 1, as V rows of up to 2^128 would take larger ones out
+// of 32 bits.  8 bits: the second product takes a weight times its row's V scale, in f16; the unit of its sums is 2^u, u set
+// kBelow under the largest logit + log2 of the V scale so far, moved when one could pass it by kHigh.  The sum of the
+// softmax keeps to m: with one reference for both, the rows beside a V row of 2^100 and more fell below 32 bits.
+constexpr float kAbove = 8.f, kHigh = 14.f, kBelow = 6.f;
 
-// A record: o [G][D] (not divided), m [G], l [G], whether any row counted; floats, a multiple of 4.
-__host__ __device__ constexpr int record_floats(int G, int D) { return G * D + (2 * G + 1 + 3) / 4 * 4; }
+// A record: o [G][D] (not divided), m [G], l [G], whether any row counted, 8 bits: u [G]; floats, a multiple of 4.
+__host__ __device__ constexpr int record_floats(int G, int D)
+{
+    return G * D + ((RA_PAGED_FMT == RA_PAGED_FP8 ? 3 : 2) * G + 1 + 3) / 4 * 4;
+}
 
 struct Work {  // the launch's tiles in a CTA's shared memory
     int32_t pre[RA_MAX_BATCH + 1];  // tiles before sequence b
@@ -251,6 +256,7 @@ struct Piece {
     float O[NH][D / 16][4];
     float R[kSplit ? NH : 1][kSplit ? D / 16 : 1][4];
     float m[NH][2], l[NH][2];
+    float u[kSplit ? 1 : NH][2], down[kSplit ? 1 : NH][2];  // down: 2^(m - u), a power of two
     int any;
     __device__ __forceinline__ void clear()
     {
@@ -265,6 +271,10 @@ struct Piece {
                 }
             m[s][0] = m[s][1] = -INFINITY;
             l[s][0] = l[s][1] = 0.f;
+            if constexpr (!kSplit) {
+                u[s][0] = u[s][1] = -INFINITY;
+                down[s][0] = down[s][1] = 1.f;
+            }
         }
         any = 0;
     }
@@ -275,7 +285,6 @@ struct Piece {
     }
     __device__ __forceinline__ void rescale(int s, int hd, float f)
     {
-        l[s][hd] *= f;
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -558,8 +567,8 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                     top[o][1] = fmaxf(top[o][1], fmaxf(s[i][o][1], s[i][o][3]));
                 }
             }
-            // The reference moves only when a weight could pass 2^kHigh.  8 bits: a weight is 2^(logit - reference) times the
-            // V scale; this lane's largest scale bounds it, and only where that is too much is each row's own looked at.
+            // The references move only when they have to.  8 bits: this lane's largest V scale bounds its rows' weights, and only
+            // where that is too much is each row's own looked at.
             float room = 0.f;
             if constexpr (FP8) {
                 int e = 0;
@@ -571,26 +580,39 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
 #pragma unroll
             for (int o = 0; o < NH; ++o)
 #pragma unroll
-                for (int hd = 0; hd < 2; ++hd) raise = raise || top[o][hd] + room > st.m[o][hd] + kHigh;
+                for (int hd = 0; hd < 2; ++hd) {
+                    raise = raise || top[o][hd] > st.m[o][hd];
+                    if constexpr (FP8) raise = raise || top[o][hd] + room > st.u[o][hd] + kHigh;
+                }
             if (__any_sync(kAll, raise)) {
 #pragma unroll
                 for (int o = 0; o < NH; ++o)
 #pragma unroll
                     for (int hd = 0; hd < 2; ++hd) {
-                        float x = top[o][hd];
+                        const float x = rows_max(top[o][hd]), m = st.m[o][hd];
+                        const float mn = x > m ? x + kAbove : m;
+                        if (mn != m) {
+                            st.l[o][hd] *= ex2(m - mn);
+                            st.m[o][hd] = mn;
+                        }
                         if constexpr (FP8) {
-                            x = -INFINITY;
+                            float y = -INFINITY;
 #pragma unroll
                             for (int i = 0; i < T / 16; ++i)
 #pragma unroll
                                 for (int e = 0; e < 2; ++e)
-                                    x = fmaxf(x, s[i][o][2 * e + hd] + (float)((__float_as_int(vs[i][e]) >> 23) - 127));
-                        }
-                        x = rows_max(x);
-                        if (x > st.m[o][hd] + (FP8 ? kBelow : kHigh)) {
-                            const float mn = x - kBelow;
-                            st.rescale(o, hd, ex2(st.m[o][hd] - mn));
-                            st.m[o][hd] = mn;
+                                    y = fmaxf(y, s[i][o][2 * e + hd] + (float)((__float_as_int(vs[i][e]) >> 23) - 127));
+                            y = rows_max(y);
+                            const float u = st.u[o][hd];
+                            if (mn != m || y > u + kBelow) {
+                                float c = rintf((y > u + kBelow ? y - kBelow : u) - mn);
+                                if (!(fabsf(c) < 126.f)) c = 0.f;  // (no finite logit; else within -75 to 115: a V scale, kBelow, kAbove)
+                                st.u[o][hd] = mn + c;
+                                st.down[o][hd] = exp2i(-(int)c);
+                                st.rescale(o, hd, ex2(u - (mn + c)));
+                            }
+                        } else if (mn != m) {
+                            st.rescale(o, hd, ex2(m - mn));
                         }
                     }
             }
@@ -612,7 +634,7 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                         st.l[o][0] += x;
                         st.l[o][1] += y;
                         if constexpr (FP8) {
-                            w[o][half] = transpose8(pack_f16(x * vs[i][half], y * vs[i][half]));
+                            w[o][half] = transpose8(pack_f16(x * vs[i][half] * st.down[o][0], y * vs[i][half] * st.down[o][1]));
                         } else {
                             const uint32_t v = pack_bf16(x, y);
                             w[o][half] = transpose8(v);
@@ -657,12 +679,18 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                 if (from_start && head_end) {  // all of it
                     const long long row0 = (long long)cur.b * H + cur.h * G;
                     float inv[NH][2];
+                    [[maybe_unused]] float up[NH][2];
 #pragma unroll
                     for (int o = 0; o < NH; ++o)
 #pragma unroll
-                        for (int hd = 0; hd < 2; ++hd) inv[o][hd] = 1.f / l[o][hd];
+                        for (int hd = 0; hd < 2; ++hd) {
+                            inv[o][hd] = 1.f / l[o][hd];
+                            if constexpr (FP8) up[o][hd] = 1.f / st.down[o][hd];
+                        }
                     st.each(lane, G, [&](int o, int hd, int head, int d, float x) {
-                        p.out[(row0 + head) * D + d] = st.any ? __bfloat16_as_ushort(__float2bfloat16_rn(x * inv[o][hd])) : (uint16_t)0;
+                        x *= inv[o][hd];
+                        if constexpr (FP8) x *= up[o][hd];  // (last: before, it could overflow where the output does not)
+                        p.out[(row0 + head) * D + d] = st.any ? __bfloat16_as_ushort(__float2bfloat16_rn(x)) : (uint16_t)0;
                     });
                     if (p.lse && gq == 0)
 #pragma unroll
@@ -683,6 +711,7 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                                 if (8 * o + 2 * t + hd < G) {
                                     rec[G * D + 8 * o + 2 * t + hd] = st.m[o][hd];
                                     rec[G * D + G + 8 * o + 2 * t + hd] = l[o][hd];
+                                    if constexpr (FP8) rec[G * D + 2 * G + 1 + 8 * o + 2 * t + hd] = st.u[o][hd];
                                 }
                     if (lane == 0) rec[G * D + 2 * G] = st.any ? 1.f : 0.f;
                 }
@@ -709,7 +738,9 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
     constexpr int kW = kJoinThreads / 32, kAtOnce = GROUP ? 4 : 8;  // loads under way per thread
     constexpr int kBlock = 512;                         // records * heads whose maxima and sums are in shared memory at a time
     __shared__ __align__(16) uint8_t shared[sizeof(Work)];
+    constexpr bool FP8 = RA_PAGED_FMT == RA_PAGED_FP8;
     __shared__ float s_m[kBlock], s_l[kBlock], s_top[kW], s_sum[kJoinThreads];
+    [[maybe_unused]] __shared__ float s_u[FP8 ? kBlock : 1], s_top_u[kW];  // (8 bits: the unit of o is 2^u)
     __shared__ float4 s_later[GROUP ? kJoinThreads : 1];
     static_assert(sizeof(Work) >= kJoinThreads * sizeof(float4), "the sums of a CTA's only head take the place of the tiles");
     Work& work = *reinterpret_cast<Work*>(shared);
@@ -743,7 +774,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
         }
         const int stride = record_floats(G, D), most = kBlock / hg;
         auto rec = [&](int i) { return p.partial + ((long long)(from + i) * 2 + (i == 0 ? 1 : 0)) * stride; };
-        float m = -INFINITY, l = 0.f;
+        float m = -INFINITY, l = 0.f, u = -INFINITY;
         bool any = false;
         float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
         for (int base = 0; base < count; base += most) {
@@ -758,7 +789,7 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
             };
             load(part);  // (before the factors they wait for)
             bool some = false;
-            float top = -INFINITY;
+            float top = -INFINITY, top_u = -INFINITY;
             for (int i = tid; i < here * hg; i += kJoinThreads) {
                 const int g = g0 + i % hg;
                 const float* r = rec(base + i / hg) + G * D;
@@ -767,24 +798,44 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
                 s_l[i] = g < G ? r[G + g] : 0.f;
                 some = some || r[2 * G] != 0.f;
                 top = fmaxf(top, mi);
+                if constexpr (FP8) {
+                    const float ui = g < G ? r[2 * G + 1 + g] : -INFINITY;
+                    s_u[i] = ui;
+                    top_u = fmaxf(top_u, ui);
+                }
             }
             if constexpr (!GROUP) {
 #pragma unroll
-                for (int y = 16; y; y >>= 1) top = fmaxf(top, __shfl_xor_sync(kAll, top, y));
-                if (lane == 0) s_top[warp] = top;
+                for (int y = 16; y; y >>= 1) {
+                    top = fmaxf(top, __shfl_xor_sync(kAll, top, y));
+                    if constexpr (FP8) top_u = fmaxf(top_u, __shfl_xor_sync(kAll, top_u, y));
+                }
+                if (lane == 0) {
+                    s_top[warp] = top;
+                    s_top_u[warp] = top_u;
+                }
             }
             any = __syncthreads_or(some) || any;
             top = m;
+            top_u = u;
             if constexpr (!GROUP) {
 #pragma unroll
-                for (int w = 0; w < kW; ++w) top = fmaxf(top, s_top[w]);
+                for (int w = 0; w < kW; ++w) {
+                    top = fmaxf(top, s_top[w]);
+                    if constexpr (FP8) top_u = fmaxf(top_u, s_top_u[w]);
+                }
             } else {
 #pragma unroll 4
-                for (int i = 0; i < here; ++i) top = fmaxf(top, s_m[i * hg + j]);
+                for (int i = 0; i < here; ++i) {
+                    top = fmaxf(top, s_m[i * hg + j]);
+                    if constexpr (FP8) top_u = fmaxf(top_u, s_u[i * hg + j]);
+                }
             }
-            const float keep = m == -INFINITY ? 0.f : ex2(m - top);
+            auto factor = [](float from, float to) { return from == -INFINITY ? 0.f : ex2(from - to); };
+            const float keep_l = factor(m, top), keep = FP8 ? factor(u, top_u) : keep_l;
             m = top;
-            l *= keep;
+            u = top_u;
+            l *= keep_l;
             if (base) {  // (a piece whose weights are all zero still carries the NaN that an infinity times them is)
                 o.x *= keep;
                 o.y *= keep;
@@ -797,8 +848,8 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
                 for (int k = 0; k < kAtOnce; ++k) {
                     const int i = i0 + k * parts;
                     if (i >= here) break;
-                    const float mi = s_m[i * hg + j], f = mi == -INFINITY ? 0.f : ex2(mi - m);
-                    l += f * s_l[i * hg + j];
+                    const float of_l = factor(s_m[i * hg + j], m), f = FP8 ? factor(s_u[i * hg + j], u) : of_l;
+                    l += of_l * s_l[i * hg + j];
                     o.x += f * x[k].x;
                     o.y += f * x[k].y;
                     o.z += f * x[k].z;
@@ -834,8 +885,9 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
             if (GROUP) __syncthreads();  // (the next head's sums come here)
         }
         if (part == 0 && live) {
+            const float up = FP8 ? ex2(u - m) : 1.f;  // (last, as in the attention)
             reinterpret_cast<uint2*>(p.out + row * D)[c] =
-                any ? make_uint2(pack_bf16(o.x / l, o.y / l), pack_bf16(o.z / l, o.w / l)) : make_uint2(0u, 0u);
+                any ? make_uint2(pack_bf16(o.x / l * up, o.y / l * up), pack_bf16(o.z / l * up, o.w / l * up)) : make_uint2(0u, 0u);
             if (p.lse && lead) p.lse[row] = any ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
         }
     } while (GROUP && (item += gridDim.x) < items);
