@@ -498,10 +498,12 @@ int ra_paged_read(ra_paged* c, int layer, uint16_t* k, uint16_t* v, int64_t row_
 
 /*
  * Attention of one new token per sequence over its lens[b] rows: out[b][qh] = sum_i softmax_i(scale * q[b][qh] .
- * k_i) v_i (fp32 accumulation, bf16 output).  q: device bf16, head qh of sequence b at b * q_row_stride + qh *
- * q_head_stride; out: device [batch][q_heads][head_dim]; lse (may be NULL): device fp32 [batch][q_heads], the
- * natural log of sum_i exp(scale * q . k_i), with which parts of one context can be joined.  scale <= 0 means
- * 1/sqrt(head_dim).  An empty sequence's output is 0, its lse -infinity.
+ * k_i) v_i, bf16 output.  Logits, the softmax's maximum and sum and the sums of values are fp32; in the product with V a
+ * weight has 16 bits (RA_PAGED_BF16) or 22 (RA_PAGED_FP8, where channels of q below 2^-31 of their row's largest keep steps of
+ * 2^-38 of it).  q: device bf16, head qh of sequence b at b * q_row_stride + qh * q_head_stride; out: device
+ * [batch][q_heads][head_dim]; lse (may be NULL): device fp32 [batch][q_heads], the natural log of sum_i exp(scale * q .
+ * k_i), with which parts of one context can be joined.  scale <= 0 means 1/sqrt(head_dim).  An empty sequence's output
+ * is 0, its lse -infinity.
  */
 int ra_paged_attn(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* out,
                   float* lse, int batch, const int32_t* lens, const int32_t* table, int table_stride, float scale,

@@ -9,7 +9,8 @@
 // tile, where its bytes take an SM several hundred clocks to fetch.
 //   bf16:  weights in two bf16 parts (nearest, and what that left out), in products of their own.
 //   8 bits: codes become f16 (exactly) in registers, queries f16 at a power of two of their row (exactly, but for
-//          channels below 2^-38 of the largest), weights f16.  A row's power-of-two scales go to its logit (K) and its
+//          channels below 2^-31 of the largest, which keep steps of 2^-38 of it), weights in two f16 parts (22 bits; with one,
+//          11 bits, values that cancel showed it).  A row's power-of-two scales go to its logit (K) and its
 //          weight (V); the unit of the sums of values follows logit + log2 of the V scale, so that a weight fits f16
 //          whatever the scale.  (8-bit operands, queries in three parts, took more instructions than the kernel then
 //          had, 808 per tile of 32 rows against 603; it has 443 now.)
@@ -634,7 +635,10 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                         st.l[o][0] += x;
                         st.l[o][1] += y;
                         if constexpr (FP8) {
-                            w[o][half] = transpose8(pack_f16(x * vs[i][half] * st.down[o][0], y * vs[i][half] * st.down[o][1]));
+                            const float xv = x * vs[i][half] * st.down[o][0], yv = y * vs[i][half] * st.down[o][1];
+                            const __half2 v = __floats2half2_rn(xv, yv);
+                            w[o][half] = transpose8(*reinterpret_cast<const uint32_t*>(&v));
+                            left[o][half] = transpose8(pack_f16(xv - __low2float(v), yv - __high2float(v)));
                         } else {
                             const uint32_t v = pack_bf16(x, y);
                             w[o][half] = transpose8(v);
@@ -654,7 +658,10 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                             const uint32_t x = __byte_perm(v[2 * j], 0, 0x3120), y = __byte_perm(v[2 * j + 1], 0, 0x3120);
                             const uint32_t a[4] = {codes_f16(x & 0xffffu), codes_f16(x >> 16), codes_f16(y & 0xffffu), codes_f16(y >> 16)};
 #pragma unroll
-                            for (int o = 0; o < NH; ++o) mma(st.O[o][c + j], a, w[o][0], w[o][1]);
+                            for (int o = 0; o < NH; ++o) {
+                                mma(st.O[o][c + j], a, w[o][0], w[o][1]);
+                                mma(st.O[o][c + j], a, left[o][0], left[o][1]);
+                            }
                         }
                     } else {
 #pragma unroll
