@@ -490,7 +490,8 @@ int ra_paged_write(ra_paged* c, int layer, const uint16_t* k, const uint16_t* v,
 
 /*
  * Read rows back as bf16, the values they are held as (exact in both formats): the same arguments, with k and v
- * written.  Each sequence's last rows[b + 1] - rows[b] tokens (all of them, for a swap or a copy).
+ * written.  Each sequence's last rows[b + 1] - rows[b] tokens (all of them, for a swap or a copy).  Strides by which
+ * two of the n_rows * kv_heads rows would share an element are refused.
  */
 int ra_paged_read(ra_paged* c, int layer, uint16_t* k, uint16_t* v, int64_t row_stride, int64_t head_stride, int batch,
                   const int32_t* rows, int n_rows, const int32_t* lens, const int32_t* table, int table_stride,

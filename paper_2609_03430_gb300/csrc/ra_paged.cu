@@ -769,7 +769,7 @@ int rows_call(ra_paged* c, int layer, const void* k, const void* v, int64_t row_
     if (n_rows == 0) return RA_OK;
     if (!k || !v || !aligned16(k) || !aligned16(v)) return fail(c, RA_ERR_INVALID_ARG, "k and v must be non-NULL and 16-byte aligned");
     if ((rc = check_strides(c, "k / v", row_stride, head_stride)) != RA_OK) return rc;
-    if (!write && ((n_rows > 1 && row_stride < c->D) || (c->KVH > 1 && head_stride < c->D)))
+    if (!write && rows_overlap(row_stride, head_stride, n_rows, c->KVH, c->D))
         return fail(c, RA_ERR_INVALID_ARG, "rows read back would overlap (strides %lld, %lld)", (long long)row_stride, (long long)head_stride);
     if (write) {
         p.k_in = (const uint16_t*)k;

@@ -116,6 +116,20 @@ __host__ __device__ inline PrefetchShare prefetch_share(unsigned grid_x, unsigne
     return PrefetchShare{cta < (unsigned long long)most ? (int)cta * threads + thread : -1, most * threads};
 }
 
+// Whether any two of n_rows x heads rows of D elements, row r of head h at r * row + h * head (neither negative), share an
+// element: row r' of head h' meets it where (h' - h) * head is within D of (r - r') * row.
+inline bool rows_overlap(long long row, long long head, int n_rows, int heads, int D)
+{
+    if ((n_rows > 1 && row < D) || (heads > 1 && head < D)) return true;
+    if (n_rows < 2 || heads < 2 || (row - D) / head >= heads - 1 || (head - D) / row >= n_rows - 1) return false;  // (whole rows or heads apart)
+    for (int dh = 1; dh < heads; ++dh) {
+        const __int128 at = (__int128)dh * head;
+        const __int128 dr = at / row, below = at - dr * row;
+        if ((dr >= 1 && dr < n_rows && below < D) || (dr + 1 < n_rows && row - below < D)) return true;
+    }
+    return false;
+}
+
 #ifdef __CUDACC__
 // Brings lines into L2 ahead of their first use (thread i of n, before the kernel waits for its predecessor: L2 is
 // where a predecessor's writes arrive, so a line fetched early is not a stale one).
