@@ -535,9 +535,20 @@ int ra_paged_sparse_attn(ra_paged* c, int layer, const uint16_t* q, int64_t q_ro
 
 /*
  * Synchronise `stream` and report (once) what the kernels flagged: RA_ERR_INVALID_ARG for device inputs out of
- * range, RA_ERR_DEVICE_TIMEOUT for a bounded wait that ran out.
+ * range, RA_ERR_DEVICE_TIMEOUT for a bounded wait that ran out (2 s for rows on their way to the attention; the heads whose
+ * rows did not arrive have NaN as outputs and lse).
  */
 int ra_paged_check(ra_paged* c, void* stream);
+
+/*
+ * Test hook of that wait: ra_paged_attn whose share `share` (the launch's rows lie in equal shares, one per warp, in order)
+ * expects 16 bytes more of its tile `tile` than it copies, with waits bounded at limit_ns nanoseconds (1 000 .. 100 000 000).
+ * The launch gives up as one whose copy was lost does, and the context stays usable.  Caches of head_dim 64, page 16 and
+ * at most 8 query heads per KV head; RA_ERR_UNSUPPORTED for others.
+ */
+int ra_paged_debug_timeout_probe(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride,
+                                 uint16_t* out, float* lse, int batch, const int32_t* lens, const int32_t* table,
+                                 int table_stride, int share, int tile, uint64_t limit_ns, void* stream);
 const char* ra_paged_last_error(const ra_paged* c);
 void ra_paged_destroy(ra_paged* c);
 

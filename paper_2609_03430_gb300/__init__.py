@@ -80,6 +80,7 @@ SIGNATURES = {
     "ra_paged_select": (_i, [_vp, _i, _vp, _i64, _i64, _i, _vp, _vp, _i, _i, _i, _i, _vp, _vp]),
     "ra_paged_sparse_attn": (_i, [_vp, _i, _vp, _i64, _i64, _vp, _vp, _i, _vp, _vp, _i, _vp, _i, ctypes.c_float, _vp]),
     "ra_paged_check": (_i, [_vp, _vp]),
+    "ra_paged_debug_timeout_probe": (_i, [_vp, _i, _vp, _i64, _i64, _vp, _vp, _i, _vp, _vp, _i, _i, _i, _u64, _vp]),
     "ra_paged_last_error": (ctypes.c_char_p, [_vp]),
     "ra_paged_destroy": (None, [_vp]),
 }
@@ -369,6 +370,13 @@ def ra_paged_sparse_attn(ctx, layer, q_ptr, q_row_stride, q_head_stride, out_ptr
 
 def ra_paged_check(ctx, stream=None):
     return _check_paged(lib().ra_paged_check(ctx, _stream_ptr(stream)), ctx)
+
+
+def ra_paged_debug_timeout_probe(ctx, layer, q_ptr, q_row_stride, q_head_stride, out_ptr, lse_ptr, batch, lens_ptr, table_ptr,
+                                 table_stride, share, tile, limit_ns, stream=None):
+    return _check_paged(lib().ra_paged_debug_timeout_probe(ctx, layer, q_ptr, q_row_stride, q_head_stride, out_ptr, lse_ptr, batch,
+                                                           lens_ptr, table_ptr, table_stride, share, tile, limit_ns,
+                                                           _stream_ptr(stream)), ctx)
 
 
 def ra_paged_last_error(ctx=None):

@@ -789,9 +789,12 @@ int rows_call(ra_paged* c, int layer, const void* k, const void* v, int64_t row_
 
 int attn_call(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* out, float* lse,
               int batch, const int32_t* lens, const int32_t* table, int table_stride, const int32_t* sel, int top, float scale,
-              void* stream)
+              void* stream, uint64_t probe_ns = 0, int probe_share = 0, int probe_tile = 0)
 {
     PagedAttnParams p{};
+    p.probe_ns = probe_ns;
+    p.probe_share = probe_share;
+    p.probe_tile = probe_tile;
     int rc = view(c, layer, batch, lens, table, table_stride, p.c);
     if (rc != RA_OK) return rc;
     if (!q || !out || !aligned16(q) || !aligned16(out)) return fail(c, RA_ERR_INVALID_ARG, "q and out must be non-NULL and 16-byte aligned");
@@ -961,6 +964,20 @@ int ra_paged_sparse_attn(ra_paged* c, int layer, const uint16_t* q, int64_t q_ro
     if (!sel || (reinterpret_cast<uintptr_t>(sel) & 3u)) return fail(c, RA_ERR_INVALID_ARG, "sel must be non-NULL and 4-byte aligned");
     if (top < 1 || top > RA_PAGED_MAX_TOP) return fail(c, RA_ERR_INVALID_ARG, "top %d out of [1, %d]", top, RA_PAGED_MAX_TOP);
     return attn_call(c, layer, q, q_row_stride, q_head_stride, out, lse, batch, lens, table, table_stride, sel, top, scale, stream);
+}
+
+int ra_paged_debug_timeout_probe(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, uint16_t* out,
+                                 float* lse, int batch, const int32_t* lens, const int32_t* table, int table_stride, int share, int tile,
+                                 uint64_t limit_ns, void* stream)
+{
+    if (!c) return fail(nullptr, RA_ERR_INVALID_ARG, "ctx is NULL");
+    if (c->D != 64 || c->page != 16 || c->G > 8)
+        return fail(c, RA_ERR_UNSUPPORTED, "the probe is built for heads of 64 channels, pages of 16 and at most 8 query heads per KV head");
+    if (limit_ns < 1000ull || limit_ns > 100000000ull)
+        return fail(c, RA_ERR_INVALID_ARG, "limit_ns %llu outside [1e3, 1e8]", (unsigned long long)limit_ns);
+    if (share < 0 || tile < 0) return fail(c, RA_ERR_INVALID_ARG, "share %d and tile %d must not be negative", share, tile);
+    return attn_call(c, layer, q, q_row_stride, q_head_stride, out, lse, batch, lens, table, table_stride, nullptr, 0, 0.f, stream, limit_ns,
+                     share, tile);
 }
 
 int ra_paged_check(ra_paged* c, void* stream)

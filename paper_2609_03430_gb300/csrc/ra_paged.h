@@ -78,6 +78,8 @@ struct PagedAttnParams {
     int top;
     float scale_log2;    // scale * log2 e
     float* partial;      // records of heads that several warps hold
+    uint64_t probe_ns;   // a test's launch: its waits' limit, and the tile of a share whose wait runs out (0: none)
+    int probe_share, probe_tile;
 };
 
 struct PagedSelectParams {

@@ -249,6 +249,25 @@ struct Cursor {
     }
 };
 
+// What a head (all of it, or its part in record `rec`) reads as when its rows did not arrive: NaN, not an earlier call's values.
+__device__ __noinline__ void lost(const PagedAttnParams& p, int lane, int D, const Cursor& head, bool whole, float* rec)
+{
+    const int G = p.c.G;
+    const long long row0 = ((long long)head.b * p.c.KVH + head.h) * G;
+    for (int i = lane; i < G * D; i += 32) {
+        if (whole) p.out[row0 * D + i] = 0x7fffu;
+        else rec[i] = NAN;
+    }
+    for (int i = lane; i < G; i += 32) {
+        if (whole && p.lse) p.lse[row0 + i] = NAN;
+        if (whole) continue;
+        rec[G * D + i] = 0.f;
+        rec[G * D + G + i] = NAN;
+        if (RA_PAGED_FMT == RA_PAGED_FP8) rec[G * D + 2 * G + 1 + i] = 0.f;
+    }
+    if (!whole && lane == 0) rec[G * D + 2 * G] = 1.f;
+}
+
 // The running state of a head's rows: NH sets of 8 query heads.  This lane (gq = lane / 4, t = lane % 4): heads 2 t and
 // 2 t + 1 of a set; of O^T's 16 channels i the rows gq and gq + 8.
 template <int D, int NH>
@@ -314,7 +333,8 @@ struct Piece {
     }
 };
 
-template <int D, int U, int NH>
+// PROBE: a test's launch, in which one tile of a share expects more bytes than are copied, so that its wait runs out.
+template <int D, int U, int NH, bool PROBE>
 __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const PagedAttnParams p)
 {
     using Geo = PagedGeo<RA_PAGED_FMT, D>;
@@ -406,7 +426,8 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
             const unsigned mask = __ballot_sync(kAll, live);
             if (lane == 0) {
                 meta[st] = 0;
-                mbar_arrive_expect_tx(&bars[st], __popc(mask) * Geo::unit_bytes(U));
+                const int never = PROBE && mine == p.probe_share && issued == p.probe_tile ? 16 : 0;
+                mbar_arrive_expect_tx(&bars[st], __popc(mask) * Geo::unit_bytes(U) + never);
             }
             __syncwarp();
             if (live) {
@@ -472,11 +493,20 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
                     }
                 }
             }
-            if (!mbar_wait_bounded(&bars[stage], parity, kWaitLimitNs)) {
-                // Give up: flag it, let the copies already issued land (bounded), leave.
+            const uint64_t limit_ns = PROBE ? p.probe_ns : kWaitLimitNs;
+            if (!__all_sync(kAll, mbar_wait_bounded(&bars[stage], parity, limit_ns))) {  // (the lanes leave together or not at all)
+                // Give up: flag it, let the copies already issued land (bounded), leave NaN for the rest of the share.
                 if (lane == 0) atomicOr(p.c.err, kDeviceErrTimeout);
                 for (int u = it + 1; u < issued; ++u)
-                    (void)mbar_wait_bounded(&bars[u % kStages], (uint32_t)((u / kStages) & 1), kWaitLimitNs);
+                    (void)mbar_wait_bounded(&bars[u % kStages], (uint32_t)((u / kStages) & 1), limit_ns);
+                for (int left = tiles - it, n; left > 0; left -= n) {
+                    n = min(cur.n - cur.t, left);
+                    lost(p, lane, D, cur, from_start && cur.t + n == cur.n,
+                         p.partial + ((long long)mine * 2 + (from_start ? 1 : 0)) * record_floats(G, D));
+                    from_start = true;
+                    cur.t += n - 1;
+                    cur.next(work, KVH, p.c.batch);
+                }
                 return;
             }
             __syncwarp();
@@ -900,13 +930,13 @@ __global__ void __launch_bounds__(kJoinThreads, 4) paged_join_kernel(const Paged
     } while (GROUP && (item += gridDim.x) < items);
 }
 
-template <int D, int U, int NH>
+template <int D, int U, int NH, bool PROBE = false>
 cudaError_t launch(const PagedAttnParams& p, int sms, cudaStream_t s)
 {
     using Geo = PagedGeo<RA_PAGED_FMT, D>;
     constexpr int stage = Geo::kTile / U * Geo::unit_stride(U);
     static_assert(smem_of(stage, kWarps<D>).total <= (int)kSmemMost, "the ring fits");
-    cudaError_t e = launch_pdl(paged_attn_kernel<D, U, NH>, dim3(sms), dim3(32 * kWarps<D>), smem_of(stage, kWarps<D>).total, s, p);
+    cudaError_t e = launch_pdl(paged_attn_kernel<D, U, NH, PROBE>, dim3(sms), dim3(32 * kWarps<D>), smem_of(stage, kWarps<D>).total, s, p);
     if (e != cudaSuccess) return e;
     const int heads = p.c.KVH * p.c.G * p.c.batch;
     if (heads > sms) {
@@ -922,7 +952,11 @@ cudaError_t launch(const PagedAttnParams& p, int sms, cudaStream_t s)
 template <int D, int U, int NH>
 cudaError_t prepare()
 {
-    return cudaFuncSetAttribute(paged_attn_kernel<D, U, NH>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
+    if (D == 64 && U == 16 && NH == 1) {
+        const cudaError_t e = cudaFuncSetAttribute(paged_attn_kernel<64, 16, 1, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaFuncSetAttribute(paged_attn_kernel<D, U, NH, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost);
 }
 
 // f(integral constants D, unit rows, sets of 8 heads) for a cache
@@ -975,6 +1009,7 @@ cudaError_t RA_PAGED_NAME(paged_attn_prepare)(int D, int page, int G)
 }
 cudaError_t RA_PAGED_NAME(launch_paged_attn)(int D, const PagedAttnParams& p, int sms, cudaStream_t s)
 {
+    if (p.probe_ns) return launch<64, 16, 1, true>(p, sms, s);  // (the caller has seen to the shape)
     return pick(D, 1 << p.c.page_shift, p.c.G, [&](auto n) { return launch_of(n, p, sms, s); });
 }
 
