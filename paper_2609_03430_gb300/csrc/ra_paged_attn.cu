@@ -169,7 +169,7 @@ __host__ __device__ constexpr Smem smem_of(int stage_bytes, int warps)
     return s;
 }
 
-// Tiles per sequence and their prefix sums, by NT threads (up to 32 sequences: by every warp for itself, all writing the same).
+// Tiles per sequence and their prefix sums, by NT threads (up to 32 sequences: by the first warp).
 template <int NT>
 __device__ __forceinline__ void count_tiles(const PagedAttnParams& p, int T, Work& work)
 {
@@ -191,10 +191,12 @@ __device__ __forceinline__ void count_tiles(const PagedAttnParams& p, int T, Wor
         return x;
     };
     if (p.c.batch <= 32) {
-        const int mine = lane < p.c.batch ? tiles_of(lane) : 0, inc = scan(mine);
-        if (lane < p.c.batch) work.pre[lane] = inc - mine;
-        if (lane == 31) work.pre[p.c.batch] = inc;
-        __syncwarp();
+        if (warp == 0) {
+            const int mine = lane < p.c.batch ? tiles_of(lane) : 0, inc = scan(mine);
+            if (lane < p.c.batch) work.pre[lane] = inc - mine;
+            if (lane == 31) work.pre[p.c.batch] = inc;
+        }
+        __syncthreads();
         return;
     }
     constexpr int per = (RA_MAX_BATCH + NT - 1) / NT;
