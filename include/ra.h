@@ -483,6 +483,11 @@ int ra_paged_bind(ra_paged* c, void* device_arena, size_t bytes, void* stream);
  * <= n_rows; NULL: row b is sequence b's newest token (n_rows = batch; an empty sequence writes nothing). Earlier
  * rows of a page must be written before later ones where bounds are kept (a write at a page's first position
  * begins its bounds anew).  Two sequences must not write one page in a call.
+ * A length may be taken back and positions written again (tokens that a check rejected, a replay).  Rows and attention
+ * know no other; bounds only widen within a page: until it is written from its first position again, its bounds are
+ * those of every key written there since it last was, dropped and replaced ones too, and a dropped key that was not finite keeps
+ * the page in ra_paged_select's second class.  Its score still bounds its keys' products; it may be chosen where the
+ * keys that are left would not have been.
  */
 int ra_paged_write(ra_paged* c, int layer, const uint16_t* k, const uint16_t* v, int64_t row_stride, int64_t head_stride,
                    int batch, const int32_t* rows, int n_rows, const int32_t* lens, const int32_t* table,
@@ -515,10 +520,11 @@ int ra_paged_attn(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_strid
  * bounds promise most, in order, as page indices within the sequence (table columns) in sel, device int32
  * [batch][kv_heads][top], filled up with -1. A page's score is, in whole numbers, sum_d sum_h (qi[h][d] > 0 ?
  * qi[h][d] * hi[d] : qi[h][d] * lo[d]) * 2^f (rounded to fp32 once): qi the group's queries in 8 bits at one
- * power-of-two scale (nearest, ties to even), lo and hi the page's lowest and highest keys as written, rounded
- * outwards to 8 bits at its power-of-two scale 2^f.  It bounds the sum over the group's heads of q . k for every
- * key of the page, up to the rounding of q.  The first `first` and last `last` pages are always taken (first +
- * last <= top), then pages holding a key that is not finite; ties go to the earlier page.  Queries that are not
+ * power-of-two scale (nearest, ties to even), lo and hi the page's lowest and highest keys as written (ra_paged_write
+ * says which keys those are where a length was taken back), rounded outwards to 8 bits at its power-of-two scale 2^f.
+ * It bounds the sum over the group's heads of q . k for every key of the page, up to the rounding of q.  The first
+ * `first` and last `last` pages are always taken (first + last <= top), then pages holding a key that is not finite;
+ * ties go to the earlier page.  Queries that are not
  * finite choose the earliest.  RA_ERR_STATE without bounds.
  */
 int ra_paged_select(ra_paged* c, int layer, const uint16_t* q, int64_t q_row_stride, int64_t q_head_stride, int batch,
