@@ -12,7 +12,7 @@ namespace ra {
 constexpr int kPagedErrInput = 4;  // value of the device error word: a length, row count or page outside its range
 constexpr int kPagedPrefetchTable = 128 << 10;  // bytes of tables that are brought into L2 ahead of their use
 constexpr int kPagedPrefetchCtas = 512;         // CTAs of a launch that bring them (a CTA per row of the largest batch)
-constexpr int kPagedMaxG = 16;     // query heads per KV head (the rows of one mma.sync operand)
+constexpr int kPagedMaxG = 16;     // query heads per KV head (two sets of 8, the columns of an mma.sync operand)
 
 // Exponents of the power-of-two scales, stored as e + 127.  8-bit rows: the smallest 2^e with max |x| <= 448 * 2^e;
 // not below 2^-60, so that the attention's sums, which carry 2^-e, stay far inside 32 bits (rows that small keep
@@ -25,14 +25,11 @@ constexpr int kScaleNaN = 255;  // the scale byte of a page that holds an infini
 // copy brings a unit: U K rows, U V rows, and in 8 bits their U + U scale bytes.  16-byte chunks of a row are
 // permuted by the row's index, the way the shared-memory reads of the tensor-core operands want them (8 rows at one chunk index hit
 // 8 different bank groups); the copy then needs no layout of its own.
-#ifndef RA_PAGED_T
-#define RA_PAGED_T(row) (row == 256 ? 32 : row == 128 ? 32 : 64)
-#endif
 template <int FMT, int D>
 struct PagedGeo {
     static constexpr int kES = FMT == RA_PAGED_FP8 ? 1 : 2;     // bytes per element
     static constexpr int kRow = D * kES;                        // bytes per row: 64, 128 or 256
-    static constexpr int kTile = RA_PAGED_T(kRow);         // rows of K and V that attention takes at a time
+    static constexpr int kTile = kRow == 64 ? 64 : 32;          // rows of K and V that attention takes at a time
     static constexpr int kScales = FMT == RA_PAGED_FP8 ? 1 : 0;  // scale bytes per row
     __host__ __device__ static constexpr int unit_rows(int page) { return page < kTile ? page : kTile; }
     __host__ __device__ static constexpr int unit_bytes(int U) { return 2 * U * (kRow + kScales); }
