@@ -152,9 +152,11 @@ __device__ __forceinline__ void prefetch_start(const PagedRowsParams& p, int D)
 // A CTA takes the rows of one page of up to 8 KV heads, a warp each; where there are too few of those for the SMs, of 2
 // heads, `split` warps per head, each every split-th set of rows.  D / 8 lanes hold a row of 8 channels each; a warp's
 // lower half takes K rows, the upper half the V rows beside them, kAtOnce sets of them under way (with 2, 4 and 8: 17k rows of
-// 10 heads written in 8 bits and read back in 59, 54 and 55 us, 65k rows of 8 heads in bf16 in 99, 90 and 93).  What
+// 10 heads written in 8 bits in 27.4, 25.6 and 25.8 us and read back in 28.3, 20.0 and 19.3; 65k rows of 8 heads in bf16 in 45.1, 44.0
+// and 42.9 and 45.2, 43.4 and 43.2; four warps a head over pages of 16 rows 32.2, 32.4 and 37.0).  What
 // bounds it is memory, each row being read once and written once, and in 8 bits the instructions of the rounding (two thirds of
-// the issue slots): those 17k rows, 132 MB, are written in 24.8 us, 0.79 of the copy rate, and read back in 19.9.
+// the issue slots): those 17k rows, 132 MB, are written in 25 us, 0.78 of the copy rate.  Keeping bounds adds 16 comparisons a lane
+// and row set and the page's own reduction: the same rows in 41 us in 8 bits and 39 in bf16 (27 without).
 constexpr int kAtOnce = 4;
 
 template <int FMT, int D>
@@ -358,8 +360,8 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const PagedRows
 
 // ---------------------------------------------------------------------------- choosing pages
 // A cluster per sequence and KV head (one CTA where there are many heads).  What bounds it is latency (one user's 516
-// pages: 6.5 us, of which 1 us until the scores begin, 1.2 the scores, 1.5 the cluster's join, 1 the cut, 0.7 the list),
-// then the 2 D + 1 bytes per page and the instructions on them (147k pages, 38 MB: 15 us).  Scores: D / 8 lanes read a
+// pages: 6 us, of which 1 us until the scores begin, 1.2 the scores, 1.5 the cluster's join, 1 the cut, 0.7 the list),
+// then, in a batch, its longest head (143k pages, 37 MB: 15 us, where the bytes take 5.4).  Scores: D / 8 lanes read a
 // page's bounds, 16 bytes each, 8 pages (D = 64: as many) under way per lane; products of 16-bit sums of queries and
 // 8-bit bounds (the sum over the heads is taken before the pages are read, so their number costs nothing).  Then the first CTA
 // finds the key that `top` pages reach, by histograms of 1024 bins over the keys that are left, from the range the keys
@@ -616,7 +618,10 @@ cudaError_t launch_rows(const PagedRowsParams& p, bool write, int sms, cudaStrea
     // every slice has a row, and a sequence's rows touch at most n / page + 2 pages
     const long long most = ((long long)p.n_rows >> p.c.page_shift) + 2ll * p.c.batch;
     const unsigned pages = (unsigned)(most < p.n_rows ? most : p.n_rows);
-    // several warps per head where there are few pages, of more than a row; the heads spread evenly over the CTAs
+    // several warps per head where there are few pages, of more than a row; the heads spread evenly over the CTAs.  With one and
+    // four warps a head: 64 page heads of 64 rows written in 8 bits in 16.9 and 5.9 us, 4096 of 128 in bf16 in 49.5 and 44.0, 5120 of 64
+    // in 8 bits in 48.5 and 46.8, 9728 in 88.0 and 84.4, 20480 in 174 and 173; of pages of 16 rows 9000 in bf16 in 22.7 and 21.9, but
+    // 10660 in 8 bits in 25.6 and 32.4 (four rows a warp): so up to 9728 (64 x 152)
     const int split = p.rows && (long long)pages * p.c.KVH < 64ll * sms ? 4 : 1, fit = kRowWarps / split;
     const int ctas = (p.c.KVH + fit - 1) / fit, heads = (p.c.KVH + ctas - 1) / ctas;
     const dim3 grid(pages, ctas);
@@ -644,8 +649,9 @@ cudaError_t launch_paged_read(int fmt, int D, const PagedRowsParams& p, int sms,
 }
 cudaError_t launch_paged_select(int D, PagedSelectParams p, int sms, cudaStream_t s)
 {
-    // a head's pages over several CTAs while all of them run at once, four on an SM (16 sequences of 8 heads: 13.0 us
-    // with two, 11.6 with four, 14.1 with eight)
+    // a head's pages over several CTAs while all of them run at once, four on an SM (by CTAs a head, 1, 2, 4 and 8: one sequence of
+    // 8 heads and 33k tokens 8.0, 7.5, 6.5 and 5.9 us; four such 8.9, 8.1, 7.2 and 7.2; 16 of up to 31k 13.2, 11.3, 10.8
+    // and 13.3; 32 of up to 64k 15.2, 15.0, 16.5 and 21.6)
     p.cluster = 1;
     while (p.cluster < kSelMostCluster && 2 * p.cluster * p.c.KVH * p.c.batch <= 4 * sms) p.cluster *= 2;
     cudaLaunchConfig_t cfg = {};

@@ -13,12 +13,12 @@
 //          11 bits, values that cancel showed it).  A row's power-of-two scales go to its logit (K) and its
 //          weight (V); the unit of the sums of values follows logit + log2 of the V scale, so that a weight fits f16
 //          whatever the scale.  (8-bit operands, queries in three parts, took more instructions than the kernel then
-//          had, 808 per tile of 32 rows against 603; it has 443 now.)
+//          had, 808 per tile of 32 rows against 603; it has 488 now.)
 // A head that lies in one share is written by its warp; the parts of the others go to records that a second kernel
 // joins, which is on the SMs by then and starts as the first one ends.
 // Measured, the join included: 1.19 GB of 48 ragged sequences in 8 bits (4 query heads per KV head) 183 us, 6.5 TB/s, 0.96
-// of a copy's rate; 1.22 GB of 32 sequences in bf16 (8 heads) 180 us, 6.8 TB/s, 1.00; 0.27 GB of one sequence of 131k rows
-// 50 us, 5.4 TB/s; one of 577 rows 7.3 us, of which 2 us pass before the first copy and 2 us in the join.
+// of a copy's rate; 1.22 GB of 32 sequences in bf16 (8 heads) 179 us, 6.8 TB/s, 1.00; 0.27 GB of one sequence of 131k rows
+// 51.5 us, 5.2 TB/s; one of 577 rows 7.3 us, of which 1.5 us pass before the first copy and 2.8 us in the join.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -39,10 +39,10 @@ namespace {
 
 constexpr unsigned kAll = 0xffffffffu;
 constexpr uint64_t kWaitLimitNs = 2000000000ull;  // bounded mbarrier waits: 2 s
-// 16 KB (bf16 rows of 128 channels) or 8 KB tiles, two per warp: 128 KB under way on an SM.  Three per warp change nothing
-// in long launches and cost short ones (131k rows of one user in 8 bits: 54.5 us with three, 52 with two).  Warps, by
-// time: 48 ragged sequences in 8 bits took 284 us with 4, 246 with 6, 195 with 8 and 203 with 12 (three tiles each, as the
-// kernel then was); 32 sequences of 9280 rows in bf16 191 with 3, 187 with 4, 190 with 6.
+// 16 KB (bf16 rows of 128 channels) or 8 KB tiles, two per warp: 128 KB under way on an SM.  With three per warp 48 ragged
+// sequences in 8 bits take 195 us (182 with two), 131k rows of one user 54 (51.6), 32 sequences of 9280 rows in bf16 185 (180).  Warps, by
+// time: the 48 sequences 256 us with 4, 197 with 6, 182 with 8, 196 with 10 and 191 with 12; the one user 55, 51.5, 51.6, 55 and 60; the 32 in bf16
+// 180 with 3, 180 with 4, 179 with 5 and 181 with 6, 16 of 2000 rows 27.5, 26.7, 28.1 and 28.2.
 constexpr int kStages = 2;
 template <int D>
 constexpr int kWarps = PagedGeo<RA_PAGED_FMT, D>::kRow == 256 ? 4 : 8;
@@ -767,7 +767,7 @@ __global__ void __launch_bounds__(32 * kWarps<D>, 1) paged_attn_kernel(const Pag
 // are few, with hundreds.  It finds its records (slot 1 of the share where the KV head starts, slot 0 of the others)
 // while the attention still runs, then sums them, each thread 4 channels of every parts-th record.  Its registers and
 // shared memory fit beside the attention's.  Also the zeros of empty slots.  What bounds it is latency, two rounds of
-// loads: 1.6 us behind the attention of one user's 577 rows (19 records a head), 4 us behind that of 131k rows (152).  (By the
+// loads: done 2.8 us after the last warp of one user's 577 rows (19 records a head), 5 us after that of 131k rows (152).  (By the
 // last CTA of a head to arrive instead, each of those steps waited for the one before: 3.7 and 8 us.)
 constexpr int kJoinThreads = 256;
 template <int D, bool GROUP>
@@ -940,6 +940,10 @@ cudaError_t launch(const PagedAttnParams& p, int sms, cudaStream_t s)
     static_assert(smem_of(stage, kWarps<D>).total <= (int)kSmemMost, "the ring fits");
     cudaError_t e = launch_pdl(paged_attn_kernel<D, U, NH, PROBE>, dim3(sms), dim3(32 * kWarps<D>), smem_of(stage, kWarps<D>).total, s, p);
     if (e != cudaSuccess) return e;
+    // Up to a head per SM each has its CTAs, up to 4 for parts of its channels; above, groups of heads share one.  Single heads and
+    // groups: 64 heads of one sequence of 131k rows in 8 bits 50.4 and 82.3 us, 128 of four of 3000 rows 11.2 and 15.0, 160 of five of 1500
+    // 11.2 and 13.5, 256 of 16 of up to 2500 15.2 and 14.7, 512 of 16 of 2000 16.0 and 15.8.  Parts, 1, 2 and 4: 32 heads of one of 4000
+    // rows 9.1, 8.1 and 8.2 us (of 577 rows 6.5, 6.6 and 6.9), 64 of one of 131k 51.3, 50.4 and 50.9, 128 of four 11.3, 12.3 and 12.2.
     const int heads = p.c.KVH * p.c.G * p.c.batch;
     if (heads > sms) {
         const int hg = p.c.G < 8 ? p.c.G : 8;
